@@ -132,6 +132,17 @@ class Engine:
         self.req_pages[rid] = have
         self.req_len[rid] = self.req_len.get(rid, 0) + tokens
 
+    def _ungrow(self, rid: int, pages, length):
+        """Back to what the request had before ``_grow`` (pages None: nothing)."""
+        have = self.req_pages.get(rid)
+        if have is not None and len(have) > (kept := 0 if pages is None else len(pages)):
+            self.alloc.free(have[kept:][::-1])  # the first one handed out is the next one again
+        for table, was in ((self.req_pages, pages), (self.req_len, length)):
+            if was is None:
+                table.pop(rid, None)
+            else:
+                table[rid] = was
+
     def _plan(self, rids, n_rows, mode):
         agents = sorted(self.resident)
         index = {a: i for i, a in enumerate(agents)}
@@ -159,20 +170,28 @@ class Engine:
 
     def run(self, rids, n_rows, q, k_new, v_new, mode):
         """Append each request's n_rows new tokens (rows in request order) and
-        attend; returns (o, lse) device tensors."""
-        for r, n in zip(rids, n_rows):
-            self._grow(r, int(n))
-        if self.rope is not None:
-            q, k_new = self.rope(q, k_new, self._positions(rids, n_rows))
-            v_new = v_new.contiguous()  # q, k_new and v_new may be views of one packed projection
-        plan = self._plan(rids, n_rows, mode)
-        o = torch.empty_like(q)
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=self.device)
-        if self.kv_format == B.PFX_KV_E4M3:
-            B.pfx_step8(self.pool, plan, k_new, v_new, q, o, lse)
-        else:
-            B.pfx_append_kv(self.pool, plan, k_new, v_new)
-            B.pfx_attention(self.pool, plan, q, o, lse)
+        attend; returns (o, lse) device tensors.  A call that raises leaves the
+        requests as they were."""
+        before = {r: (self.req_pages.get(r), self.req_len.get(r)) for r in rids}
+        try:
+            for r, n in zip(rids, n_rows):
+                self._grow(r, int(n))
+            if self.rope is not None:
+                q, k_new = self.rope(q, k_new, self._positions(rids, n_rows))
+                v_new = v_new.contiguous()  # q, k_new and v_new may be views of one packed projection
+            plan = self._plan(rids, n_rows, mode)
+            o = torch.empty_like(q)
+            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=self.device)
+            if self.kv_format == B.PFX_KV_E4M3:
+                B.pfx_step8(self.pool, plan, k_new, v_new, q, o, lse)
+            else:
+                B.pfx_append_kv(self.pool, plan, k_new, v_new)
+                B.pfx_attention(self.pool, plan, q, o, lse)
+        except BaseException:
+            # A refused call appends nothing: its tokens and pages do not count.
+            for r, (pages, length) in reversed(before.items()):
+                self._ungrow(r, pages, length)
+            raise
         self._last_plan = plan
         return o, lse
 
@@ -181,8 +200,16 @@ class Engine:
         (causal) against its agent's resident prefix."""
         if agent >= 0 and agent not in self.resident:
             raise RuntimeError(f"request {rid}: agent {agent}'s prefix is not resident")
+        was = self.req_agent.get(rid)
         self.req_agent[rid] = agent
-        return self.run([rid], [q.shape[0]], q, k_new, v_new, B.PFX_MODE_EXTEND)
+        try:
+            return self.run([rid], [q.shape[0]], q, k_new, v_new, B.PFX_MODE_EXTEND)
+        except BaseException:
+            if was is None:
+                self.req_agent.pop(rid)
+            else:
+                self.req_agent[rid] = was
+            raise
 
     def decode(self, rids, q, k_new, v_new):
         """One decode step: one new token per request."""
