@@ -162,11 +162,15 @@ class Engine:
                                  kv_format=self.kv_format).upload(device=self.device)
 
     def _positions(self, rids, n_rows):
-        """Position of every new token: behind its agent's prefix and the request's earlier tokens."""
+        """Position of every new token: behind its agent's prefix and the request's earlier tokens.  They go up from
+        pinned memory: a copy from pageable memory waits for the stream's earlier work."""
         parts = [np.arange(self.req_len[r] - n, self.req_len[r], dtype=np.int32)
                  + (self.prefix_len[self.req_agent[r]] if self.req_agent[r] >= 0 else 0)
                  for r, n in zip(rids, map(int, n_rows))]
-        return torch.from_numpy(np.concatenate(parts).astype(np.int32)).to(self.device)
+        host = torch.from_numpy(np.concatenate(parts).astype(np.int32))
+        if torch.device(self.device).type == "cpu":
+            return host
+        return host.pin_memory().to(self.device, non_blocking=True)
 
     def run(self, rids, n_rows, q, k_new, v_new, mode):
         """Append each request's n_rows new tokens (rows in request order) and
