@@ -367,10 +367,14 @@ def _call_stream(stream, *tensors):
 
 def _check_rows(plan: Plan, which: int, a, b, lse=None):
     """A pair of row tensors of a call (0: k_new, v_new; 1: q, o): consecutive bf16 rows, enough for the plan.  A view
-    of a packed projection has them apart, and would be read as other values."""
+    of a packed projection has them apart, and would be read as other values.  Those of a plan without query rows may be
+    None."""
     n = plan.sizes[which]
-    if not (a.dtype is _BF16 and b.dtype is _BF16 and a.is_contiguous() and b.is_contiguous() and a.numel() >= n
-            and b.numel() >= n):
+    if a is None or b is None:
+        if n:
+            raise ValueError(f"rows must be contiguous bf16 of at least {n} values")
+    elif not (a.dtype is _BF16 and b.dtype is _BF16 and a.is_contiguous() and b.is_contiguous() and a.numel() >= n
+              and b.numel() >= n):
         raise ValueError(f"rows must be contiguous bf16 of at least {n} values")
     if lse is not None and not (lse.dtype is _FP32 and lse.is_contiguous() and lse.numel() >= plan.sizes[2]):
         raise ValueError(f"lse must be contiguous float32 of at least {plan.sizes[2]} values")
@@ -378,15 +382,14 @@ def _check_rows(plan: Plan, which: int, a, b, lse=None):
 
 def pfx_append_kv8(pool: pfx_pool8, plan: Plan, k_new, v_new, stream=None):
     _check_rows(plan, 0, k_new, v_new)
-    rc = LIB.pfx_append_kv8(pool, plan.h, k_new.data_ptr(), v_new.data_ptr(), _call_stream(stream, k_new, v_new))
+    rc = LIB.pfx_append_kv8(pool, plan.h, _ptr(k_new), _ptr(v_new), _call_stream(stream, k_new, v_new))
     if rc:
         _check(rc)
 
 
 def pfx_attention8(pool: pfx_pool8, plan: Plan, q, o, lse=None, sm_scale: float = 0.0, stream=None):
     _check_rows(plan, 1, q, o, lse)
-    rc = LIB.pfx_attention8(pool, plan.h, q.data_ptr(), o.data_ptr(), None if lse is None else lse.data_ptr(), sm_scale,
-                            _call_stream(stream, q, o, lse))
+    rc = LIB.pfx_attention8(pool, plan.h, _ptr(q), _ptr(o), _ptr(lse), sm_scale, _call_stream(stream, q, o, lse))
     if rc:
         _check(rc)
 
@@ -394,8 +397,7 @@ def pfx_attention8(pool: pfx_pool8, plan: Plan, q, o, lse=None, sm_scale: float 
 def pfx_step8(pool: pfx_pool8, plan: Plan, k_new, v_new, q, o, lse=None, sm_scale: float = 0.0, stream=None):
     _check_rows(plan, 0, k_new, v_new)
     _check_rows(plan, 1, q, o, lse)
-    rc = LIB.pfx_step8(pool, plan.h, k_new.data_ptr(), v_new.data_ptr(), q.data_ptr(), o.data_ptr(),
-                       None if lse is None else lse.data_ptr(), sm_scale,
+    rc = LIB.pfx_step8(pool, plan.h, _ptr(k_new), _ptr(v_new), _ptr(q), _ptr(o), _ptr(lse), sm_scale,
                        _call_stream(stream, k_new, v_new, q, o, lse))
     if rc:
         _check(rc)
