@@ -1,0 +1,46 @@
+"""Rules of plans over the 8-bit pool that differ from the bf16 pool's, because the kernels do."""
+
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+pytest.importorskip("torch")
+
+import kv8_cases as KC  # noqa: E402
+from paper_2608_25523_amd import binding as B  # noqa: E402
+
+
+def plan8(hq, hkv, d, prefix_len, reqs, **kw):
+    b = KC.batch(1, hq, hkv, d, prefix_len, reqs)
+    return B.plan_from_batch(B.make_pool8(b.num_pages, hkv, d), b, kv_format=B.PFX_KV_E4M3, **kw)
+
+
+@pytest.mark.parametrize("agents,prefix,reqs", [(1, 2048, 64), (4, 8192, 32), (4, 10000, 16), (2, 4096, 56)])
+def test_decode_pieces_fit_the_chip_at_head_dim_64(agents, prefix, reqs):
+    """decode8_kernel<64> has 148 registers: three workgroups a compute unit, 768 at once.  Where pieces of 16 steps
+    are no more than that, a shorter length must not make them more."""
+    batch = (32, 8, 64, [prefix] * agents, [(i % agents, 64 + 7 * i % 449, 1) for i in range(reqs)])
+    fixed, auto = (plan8(*batch, **kw).stats().num_decode_pieces for kw in (dict(piece_steps=16), {}))
+    longest = plan8(*batch, piece_steps=64).stats().num_decode_pieces
+    assert longest <= 768, "the batch fits at some length"
+    assert auto <= max(768, fixed), (auto, fixed)
+
+
+def test_registers_behind_the_rule(tmp_path):
+    """The figure the rule stands on, from the compiler: above 128 registers and up to 168, three waves a SIMD."""
+    import os
+    import re
+    import subprocess
+    hipcc = "/opt/rocm/bin/hipcc"
+    if not os.path.exists(hipcc):
+        pytest.skip("hipcc not available")
+    from paper_2608_25523_amd.build import FLAGS, HERE, ROOT
+    out = tmp_path / "k.s"
+    subprocess.run([hipcc, *[f for f in FLAGS if f not in ("-shared", "-fPIC")], "-S", "--cuda-device-only", "-I",
+                    os.path.join(ROOT, "include"), os.path.join(HERE, "csrc", "pfx_kv8.hip"), "-o", str(out)],
+                   check=True, capture_output=True)
+    waves = {}
+    for name, body in re.findall(r"\.globl\s+(\S*decode8_kernel\S*).*?; Kernel info:(.*?)\.text", out.read_text(), re.S):
+        waves[re.search(r"ILi(\d+)E", name).group(1)] = int(re.search(r"; Occupancy: (\d+)", body).group(1))
+    assert waves == {"64": 3, "128": 2}, waves
