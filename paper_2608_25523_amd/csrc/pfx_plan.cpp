@@ -516,8 +516,9 @@ extern "C" int pfx_plan_create(const pfx_pool* pool, const pfx_prefix_table* pt,
     for (const DItem& x : dit) wide |= x.wide != 0;
     const bool three = wide || engine == PFX_DECODE_VALU || format == PFX_KV_E4M3;
     int64_t room = p->d == 128 ? kResident128 : three ? kResident64Three : kResident64;
-    // Beside extend blocks, which take longer, the pieces stay long.
-    for (int32_t r = 0; r < R && room > 0; ++r)
+    // Beside extend blocks, which take longer, the pieces stay long (in one
+    // launch with them: not those of an 8-bit pool).
+    for (int32_t r = 0; r < R && room > 0 && format == PFX_KV_BF16; ++r)
       if (p->req[r].n > 0 && !is_decode_class(r)) room = 0;
     int32_t least = format == PFX_KV_E4M3 ? kLeastPieceSteps8 : kLeastPieceSteps;
     for (int32_t r = 0; r < R; ++r) {
@@ -744,13 +745,22 @@ extern "C" int pfx_plan_create(const pfx_pool* pool, const pfx_prefix_table* pt,
     return xbs[x].cost > xbs[y].cost;
   });
   const size_t nitems = xbs.size() * size_t(hkv);
+  // Decode pieces in the extend blocks' launch.  Over an 8-bit pool they run in
+  // one of their own after it, and neither the blocks nor the pieces make room for
+  // the other.  us an attention call with the bf16 launch's rules and without,
+  // Hq 32, Hkv 8: 300 rows over 4096 keys and 8 decode requests 54.7 and 52.8
+  // (d = 128), 45.2 and 39.9 (d = 64); 1200 over 2048 and 32 requests 106.6 and
+  // 104.6, 77.5 and 65.9; 1999 over 2048 and 4 134.8 and 125.3, 91.2 and 85.3; 32
+  // over 4096 and 16 33.2 and 32.7, 26.8 and 26.6; with 64 or 128 requests, whose
+  // pieces left no room, the same.
+  const int64_t beside = format == PFX_KV_BF16 ? int64_t(npcs) : 0;
   // When no compute unit runs more than two blocks, workgroup i shares one with
   // workgroup 256 + i: the second 256 go shortest first, so that the longest
   // block has the shortest beside it.  504 blocks, 1999 rows over 2048 keys:
   // 107.1 -> 103.4 us a step call at d = 128, 74.9 -> 73.8 at d = 64; 2000 rows
   // over 16 keys 57.2 -> 54.7; where the lengths hardly differ nothing changes.
   // (Beside decode pieces the launch is fuller than that.)
-  if (int64_t(nitems) > kComputeUnits && int64_t(nitems) <= kResidentExtend && npcs == 0 && kComputeUnits % hkv == 0)
+  if (int64_t(nitems) > kComputeUnits && int64_t(nitems) <= kResidentExtend && beside == 0 && kComputeUnits % hkv == 0)
     std::reverse(xrank.begin() + kComputeUnits / hkv, xrank.end());
   if (nitems + wide_order.size() > size_t(INT32_MAX))
     return delete p, fail(PFX_ERANGE, "pfx_plan_create: too many extend blocks");
@@ -802,7 +812,7 @@ extern "C" int pfx_plan_create(const pfx_pool* pool, const pfx_prefix_table* pt,
       // pieces in two rounds, where all blocks cut in two are too many for one
       // (304 blocks: 1200 rows over 8192 keys 235 -> 188 us a step call, two
       // requests of 600 over 6000 174 -> 145).
-      for (int64_t room : {kResidentExtend, kResidentExtend - int64_t(npcs), kComputeUnits, 2 * kResidentExtend}) {
+      for (int64_t room : {kResidentExtend, kResidentExtend - beside, kComputeUnits, 2 * kResidentExtend}) {
         if (room < kComputeUnits || fixed_division) continue;
         int64_t c = std::max<int64_t>(kLeastChunkPairs, (pairs + room - 1) / room), count = 0, slots = 0;
         for (; c < longest; c += 1 + c / 32) {  // finer steps would change a piece by less than 3%
@@ -817,7 +827,7 @@ extern "C" int pfx_plan_create(const pfx_pool* pool, const pfx_prefix_table* pt,
         if (c >= longest) continue;
         const double t = (count > kResidentExtend ? 2.0 * double(c) : time(double(c), count > kComputeUnits ? double(c) : 0)) +
                          cost.fixed + cost.slot * double(slots) +
-                         (npcs && count + int64_t(npcs) > kResidentExtend ? cost.late : 0);
+                         (beside && count + beside > kResidentExtend ? cost.late : 0);
         if (t < best) {
           best = t;
           cut = static_cast<int32_t>(c);

@@ -44,3 +44,27 @@ def test_registers_behind_the_rule(tmp_path):
     for name, body in re.findall(r"\.globl\s+(\S*decode8_kernel\S*).*?; Kernel info:(.*?)\.text", out.read_text(), re.S):
         waves[re.search(r"ILi(\d+)E", name).group(1)] = int(re.search(r"; Occupancy: (\d+)", body).group(1))
     assert waves == {"64": 3, "128": 2}, waves
+
+
+def cut_bytes(batch, **kw):
+    """Workspace that the pieces of cut extend blocks take: what a plan has over one of whole blocks with the same
+    decode pieces."""
+    auto = plan8(*batch, **kw)
+    for steps in range(1, 65):
+        whole = plan8(*batch, piece_steps=steps)
+        same = [(s.num_decode_pieces, s.num_partial_rows) for s in (auto.stats(), whole.stats())]
+        if same[0] == same[1]:
+            return auto.workspace_bytes() - whole.workspace_bytes()
+    raise AssertionError("no fixed length gives the same decode pieces")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows,prefix,decode", [(300, 4096, 8), (1200, 2048, 32), (32, 4096, 16)])
+def test_extend_blocks_and_decode_pieces_plan_apart(d, rows, prefix, decode):
+    """They run in launches of their own: a mixed batch is cut as its two halves are."""
+    prompt = [(0, rows, rows)]
+    steps = [(0, 64 + 13 * i % 300, 1) for i in range(decode)]
+    mixed, alone = cut_bytes((32, 8, d, [prefix], prompt + steps)), cut_bytes((32, 8, d, [prefix], prompt))
+    assert abs(mixed - alone) <= 1024, (mixed, alone)  # sections are rounded up to 256 bytes
+    counts = [plan8(32, 8, d, [prefix], r).stats().num_decode_pieces for r in (prompt + steps, steps)]
+    assert counts[0] == counts[1], counts
