@@ -121,7 +121,11 @@ constexpr int32_t kLeastChunkPairs = 4;
 // 12.4 -> 11.6 (d = 128) and 11.3 -> 9.0 (Hq 8, Hkv 2, d = 64); over 500 (9
 // pairs) 19.2 -> 19.8 and, Hq 32, d = 64, 16.4 -> 15.7; over 700 (12) 22.6 ->
 // 23.4 and 19.1 -> 18.4; 512 rows over 2048 at Hq 64 (40) 59.0 -> 61.3: the
-// line is that of d = 128.  Cut launches gain about 1.5 us by it.
+// line is that of d = 128.  Cut launches gain about 1.5 us by it.  Not over an
+// 8-bit pool, whose append is a launch of its own: us an attention call with the
+// table and without, 4 requests of 32 rows over 128 keys 9.3 and 9.0 (d = 128),
+// 7.3 and 6.9 (d = 64), over 400 14.8 and 14.5, 11.4 and 10.9; 8 of 100 over 300
+// 17.8 and 17.6.
 constexpr int32_t kShortPairs = 8;
 struct ChunkCosts {
   double alone, fixed, slot, late;
@@ -834,7 +838,7 @@ extern "C" int pfx_plan_create(const pfx_pool* pool, const pfx_prefix_table* pt,
         }
       }
     }
-    if (cut || (int64_t(nitems) < kResidentExtend && longest <= kShortPairs)) {
+    if (cut || (format == PFX_KV_BF16 && int64_t(nitems) < kResidentExtend && longest <= kShortPairs)) {
       for (int32_t xi : xrank) {
         const int32_t steps = xsteps(xbs[xi]), n = (steps + 1) / 2, k = cut ? (n + cut - 1) / cut : 1;
         for (int32_t i = 0; i < k; ++i)

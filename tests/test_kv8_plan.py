@@ -68,3 +68,15 @@ def test_extend_blocks_and_decode_pieces_plan_apart(d, rows, prefix, decode):
     assert abs(mixed - alone) <= 1024, (mixed, alone)  # sections are rounded up to 256 bytes
     counts = [plan8(32, 8, d, [prefix], r).stats().num_decode_pieces for r in (prompt + steps, steps)]
     assert counts[0] == counts[1], counts
+
+
+@pytest.mark.parametrize("batch", [(8, 2, 64, [128], [(0, 32, 32)] * 4), (32, 8, 128, [400], [(0, 32, 32)] * 3),
+                                   (4, 4, 128, [], [(-1, 20, 20)])])
+def test_whole_extend_blocks_take_no_pieces_table(batch):
+    """The table lets the append ride in the extend launch, which no 8-bit launch does: the workspace holds the plan's
+    other sections and no more."""
+    plan = plan8(*batch)
+    s = plan.stats()
+    assert s.num_decode_pieces == 0 and s.num_extend_items > 0
+    size = [plan.export(i).size * 4 for i in (0, 1, 8, 2)] + [4 * s.num_tokens, plan.export(4).size * 4]
+    assert plan.workspace_bytes() == sum((x + 255) // 256 * 256 for x in size)
