@@ -418,7 +418,10 @@ int pfx_append_kv8(const pfx_pool8* pool, const pfx_plan* plan, const void* k_ne
  * the product with V.  A NaN in the pool makes NaN of the rows that see it and
  * of no other.  Scores (sm_scale * q . k) stay below 2^30 in magnitude: past
  * that their fp32 spacing exceeds what the softmax can take, and rows become
- * NaN. */
+ * NaN.  The largest |V| times the row's number of keys stays below 2^119: the
+ * fp32 sums hold probabilities of up to 2^8 times V until they are divided by
+ * the probabilities' sum, and past that they may overflow to infinities (the
+ * format itself holds magnitudes of up to 2^127). */
 int pfx_attention8(const pfx_pool8* pool, const pfx_plan* plan, const void* q, void* o, float* lse,
                    float sm_scale, void* hip_stream);
 

@@ -1,4 +1,5 @@
-"""The 8-bit attention kernels over long key ranges and at real sizes, against the fp64 oracle.
+"""The 8-bit attention kernels over long key ranges, at real sizes and next to the largest values they take, against the
+fp64 oracle.
 
 A wave of an extend block holds the page ids of its next 128 pages (2048 keys) and asks for more as it goes: the
 prefixes here take more, with odd page counts, so that a half step shifts the table from the suffix on."""
@@ -124,3 +125,37 @@ def test_large_decode_batch_against_fp64():
     # would change the row by 1 / sqrt(2300) = 2^-5.6.
     assert (np.linalg.norm(x - y, axis=2) <= 2.0 ** -7 * np.linalg.norm(x, axis=2)).all()
     assert np.max(np.abs(lse - other[1])) <= 2.0 ** -12
+
+
+@pytest.mark.parametrize("name,reqs", [("decode", [(0, 600, 1), (-1, 900, 1)]), ("extend", [(0, 40, 40), (-1, 900, 33)])])
+def test_values_at_the_end_of_the_range(name, reqs):
+    """max |V| times a row's keys just below 2^119: sums of probabilities of up to 2^8 stay finite.  All keys alike, whose
+    sums are the largest, but for those that a kernel takes first (extend blocks the first ones, decode waves the last),
+    7.5 lower in log2, from which the running maximum does not move."""
+    announce(f"values near 2^119 / keys, {name}")
+    d, prefix = 128, 1000
+    keys = prefix + max(r[1] for r in reqs)
+    b = KC.batch(71, 4, 1, d, [prefix], reqs)
+    top = 2.0 ** np.floor(np.log2(2.0 ** 119 / keys))
+    n = b.num_pages
+    k, v = np.zeros((n, 1, 16, d)), np.full((n, 1, 16, d), top)
+    k[..., 0] = 1.0
+    for pages in list(b.prefix_pages) + list(b.suffix_pages):
+        k[pages[:4], ..., 0] = 0.0
+        k[pages[-9:], ..., 0] = 0.0
+    v[..., 64:] *= np.where(np.random.default_rng(72).random(v[..., 64:].shape) < 0.9, 1.0, -0.5)
+    t = [torch.from_numpy(W.bf16_round(x.astype(np.float32)).view(np.int16)).cuda().view(torch.bfloat16) for x in (k, v)]
+    p8 = [torch.zeros((n, 1, w), dtype=torch.uint8, device="cuda") for w in (16 * d, 16 * d, 2)]
+    pool = B.make_pool8(n, 1, d, *p8)
+    ids = np.arange(n, dtype=np.int32)
+    ws = torch.empty(B.pfx_page_quantize_workspace_bytes(n) + 256, dtype=torch.uint8, device="cuda")
+    B.pfx_page_quantize(pool, B.make_pool(n, 1, d, *t), ids, ids, ws)
+    B.pfx_sync_check()
+    case = OnPool(b, 73)
+    q = np.zeros(case.q.shape, np.float32)
+    q[..., 0] = 7.5 * np.log(2.0) * np.sqrt(d)
+    case.q = W.bf16_round(q)
+    for kw in ({}, dict(piece_steps=64), dict(piece_steps=2)):
+        o, lse = case.attend(pool, **kw)
+        assert np.isfinite(bf16_bits_to_f64(o)).all()
+        KC.check(o, lse, case.reference([x.cpu().numpy() for x in p8]), f"{name} {kw}")
