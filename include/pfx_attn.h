@@ -472,8 +472,10 @@ int pfx_page_copy8(const pfx_pool8* dst, const pfx_pool8* src, const int32_t* ds
  *   [rotary_dim / 2], 8-byte aligned (NULL when rotary_dim is 0);
  * q_weight, k_weight: device bf16 [head_dim], 16-byte aligned, or NULL: no norm
  *   of the queries / keys.
- * The sum of squares is taken in fp32: a head in which it overflows
- * (magnitudes of 2^60 and more) becomes zero.
+ * The sum of squares is taken in fp32: with an eps of 2^-90 or more a head in
+ * which it overflows (magnitudes of 2^60 and more) becomes zero.  With a smaller
+ * one, 0 too, heads of every finite magnitude are normed (all zeros with eps = 0
+ * give NaN, as 0 / 0 does).
  * head_dim 64 or 128; rotary_dim a multiple of 16 up to head_dim
  * (PFX_EUNSUPPORTED otherwise); num_tokens below 2^24 (PFX_ERANGE).  q (and q_out) may be NULL when num_q_heads is
  * 0, k (and k_out) when num_kv_heads is 0.
