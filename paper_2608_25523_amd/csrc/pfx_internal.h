@@ -224,6 +224,9 @@ namespace pfx {
 // Thread-local error text, set by every failing entry point.
 int fail(int code, const char* fmt, ...);
 void clear_error();
+// In a catch block of an entry point: the status of what was thrown (host
+// memory that ran out), so that nothing leaves the library as an exception.
+int fail_exception(const char* who);
 // Device pointers of the plan's tables and partial states in a copy of its
 // workspace image at `base` (the uploaded workspace by default).
 // The plan in a workspace of `bytes` bytes.

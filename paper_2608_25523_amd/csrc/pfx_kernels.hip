@@ -2080,7 +2080,7 @@ extern "C" int pfx_merge_states(const float* o_parts, const float* lse_parts, in
 extern "C" size_t pfx_page_copy_workspace_bytes(int32_t n) { return n <= 0 ? 256 : (size_t(n) * 8 + 255) & ~size_t(255); }
 
 extern "C" int pfx_page_copy(const pfx_pool* dst, const pfx_pool* src, const int32_t* dst_pages,
-                             const int32_t* src_pages, int32_t n, void* ws, size_t ws_bytes, void* stream) {
+                             const int32_t* src_pages, int32_t n, void* ws, size_t ws_bytes, void* stream) try {
   if (!dst || !src) return fail(PFX_EINVAL, "pfx_page_copy: pool descriptor is NULL");
   if (n < 0) return fail(PFX_ERANGE, "pfx_page_copy: n %d < 0", n);
   if (n == 0) return PFX_OK;
@@ -2090,6 +2090,7 @@ extern "C" int pfx_page_copy(const pfx_pool* dst, const pfx_pool* src, const int
   if (dst->num_kv_heads != src->num_kv_heads || dst->head_dim != src->head_dim || dst->num_kv_heads < 1 ||
       dst->head_dim < 8 || dst->head_dim % 8)
     return fail(PFX_EINVAL, "pfx_page_copy: source and destination page formats differ");
+  if (dst->num_pages < 0 || src->num_pages < 0) return fail(PFX_ERANGE, "pfx_page_copy: num_pages < 0");
   if (!dst->k_pages || !dst->v_pages || !src->k_pages || !src->v_pages)
     return fail(PFX_EINVAL, "pfx_page_copy: page pointers are NULL");
   if (reinterpret_cast<uintptr_t>(ws) % 256) return fail(PFX_EINVAL, "pfx_page_copy: workspace not 256-byte aligned");
@@ -2146,6 +2147,8 @@ extern "C" int pfx_page_copy(const pfx_pool* dst, const pfx_pool* src, const int
     if (rc) return rc;
   }
   return PFX_OK;
+} catch (...) {
+  return fail_exception("pfx_page_copy");
 }
 
 extern "C" int pfx_sync_check(void* stream) {

@@ -1366,8 +1366,8 @@ int with_pages(const char* who, const PageSide& dst, const PageSide& src, const 
   };
   if (std::max(dst.num_pages, src.num_pages) <= 65536) run(PagesHere16{}); else run(PagesHere32{});
   return check_launch(who);
-} catch (const std::bad_alloc&) {
-  return fail(PFX_ENOMEM, "%s: host allocation failed", who);
+} catch (...) {
+  return fail_exception(who);
 }
 
 }  // namespace

@@ -5,7 +5,9 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <memory>
 #include <new>
+#include <stdexcept>
 #include <unordered_map>
 #include <vector>
 
@@ -13,19 +15,32 @@
 
 namespace pfx {
 
-static thread_local std::string g_err;
+// A fixed buffer: the message of a failed allocation allocates nothing.
+static thread_local char g_err[512];
 
 int fail(int code, const char* fmt, ...) {
-  char buf[512];
+  char buf[sizeof(g_err)];  // an argument may be the last message
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(buf, sizeof(buf), fmt, ap);
   va_end(ap);
-  g_err = buf;
+  std::memcpy(g_err, buf, std::strlen(buf) + 1);
   return code;
 }
 
-void clear_error() { g_err.clear(); }
+int fail_exception(const char* who) {
+  try {
+    throw;
+  } catch (const std::bad_alloc&) {
+    return fail(PFX_ENOMEM, "%s: host allocation failed", who);
+  } catch (const std::length_error&) {
+    return fail(PFX_ENOMEM, "%s: host allocation failed", who);
+  } catch (...) {
+    return fail(PFX_EINVAL, "%s: failed on the host", who);
+  }
+}
+
+void clear_error() { g_err[0] = 0; }
 
 // One host image kept per thread for the next plan (see pfx_plan_destroy).
 static std::vector<unsigned char>& spare_blob() {
@@ -178,7 +193,7 @@ using pfx::fail;
 
 extern "C" int pfx_version(void) { return PFX_VERSION; }
 
-extern "C" const char* pfx_last_error(void) { return pfx::g_err.c_str(); }
+extern "C" const char* pfx_last_error(void) { return pfx::g_err; }
 
 // ---------------------------------------------------------------------------
 // Page allocator
@@ -190,18 +205,19 @@ struct pfx_alloc {
   std::vector<uint8_t> used;
 };
 
-extern "C" int pfx_alloc_create(int32_t num_pages, pfx_alloc** out) {
+extern "C" int pfx_alloc_create(int32_t num_pages, pfx_alloc** out) try {
   if (!out) return fail(PFX_EINVAL, "pfx_alloc_create: out is NULL");
   *out = nullptr;
   if (num_pages < 0) return fail(PFX_ERANGE, "pfx_alloc_create: num_pages %d < 0", num_pages);
-  pfx_alloc* a = new (std::nothrow) pfx_alloc;
-  if (!a) return fail(PFX_ENOMEM, "pfx_alloc_create: host allocation failed");
+  auto a = std::make_unique<pfx_alloc>();
   a->num_pages = num_pages;
   a->free_list.resize(num_pages);
   for (int32_t i = 0; i < num_pages; ++i) a->free_list[i] = num_pages - 1 - i;
   a->used.assign(num_pages, 0);
-  *out = a;
+  *out = a.release();
   return PFX_OK;
+} catch (...) {
+  return pfx::fail_exception("pfx_alloc_create");
 }
 
 extern "C" int pfx_alloc_pages(pfx_alloc* a, int32_t n, int32_t* out_ids) {
@@ -219,7 +235,7 @@ extern "C" int pfx_alloc_pages(pfx_alloc* a, int32_t n, int32_t* out_ids) {
   return PFX_OK;
 }
 
-extern "C" int pfx_free_pages(pfx_alloc* a, const int32_t* ids, int32_t n) {
+extern "C" int pfx_free_pages(pfx_alloc* a, const int32_t* ids, int32_t n) try {
   if (!a) return fail(PFX_EINVAL, "pfx_free_pages: allocator is NULL");
   if (n < 0) return fail(PFX_ERANGE, "pfx_free_pages: n %d < 0", n);
   if (n > 0 && !ids) return fail(PFX_EINVAL, "pfx_free_pages: ids is NULL");
@@ -234,9 +250,11 @@ extern "C" int pfx_free_pages(pfx_alloc* a, const int32_t* ids, int32_t n) {
   }
   for (int32_t i = 0; i < n; ++i) {
     a->used[ids[i]] = 0;
-    a->free_list.push_back(ids[i]);
+    a->free_list.push_back(ids[i]);  // its room is there: it held every page
   }
   return PFX_OK;
+} catch (...) {
+  return pfx::fail_exception("pfx_free_pages");
 }
 
 extern "C" int pfx_alloc_num_free(const pfx_alloc* a, int32_t* out) {
@@ -271,7 +289,7 @@ bool is_group_supported(int32_t g) { return g == 1 || g == 2 || g == 4 || g == 8
 }  // namespace
 
 extern "C" int pfx_plan_create(const pfx_pool* pool, const pfx_prefix_table* pt, const pfx_batch* b,
-                               int32_t hq, int32_t mode, const pfx_plan_opts* opts, pfx_plan** out) {
+                               int32_t hq, int32_t mode, const pfx_plan_opts* opts, pfx_plan** out) try {
   using namespace pfx;
   if (!out) return fail(PFX_EINVAL, "pfx_plan_create: out is NULL");
   *out = nullptr;
@@ -385,8 +403,8 @@ extern "C" int pfx_plan_create(const pfx_pool* pool, const pfx_prefix_table* pt,
       if ((rc = claim(b->suffix_page_ids[i], "request", r))) return rc;
 
   // ---- build ----
-  pfx_plan* p = new (std::nothrow) pfx_plan;
-  if (!p) return fail(PFX_ENOMEM, "pfx_plan_create: host allocation failed");
+  auto owned = std::make_unique<pfx_plan>();
+  pfx_plan* const p = owned.get();
   p->num_pages = pool->num_pages;
   p->hkv = hkv;
   p->d = pool->head_dim;
@@ -586,7 +604,7 @@ extern "C" int pfx_plan_create(const pfx_pool* pool, const pfx_prefix_table* pt,
     }
   }
   if (part_units * G > (int64_t(1) << 31) / std::max(1, p->d))
-    return delete p, fail(PFX_ERANGE, "pfx_plan_create: too many partial rows");
+    return fail(PFX_ERANGE, "pfx_plan_create: too many partial rows");
   p->num_part_rows = part_units * G;
   // When every (merge row, KV head) has the same number of parts P, its
   // slots start at (row * Hkv + h) * P, and the merge launch computes that
@@ -686,7 +704,7 @@ extern "C" int pfx_plan_create(const pfx_pool* pool, const pfx_prefix_table* pt,
   for (int32_t k : wide_order) wide_steps += pcs[k].s1 - pcs[k].s0;
   p->deal_wide = p->num_decode_steps - wide_steps >= wide_steps;
   if (nsegs > size_t(INT32_MAX) || wide_order.size() > size_t(INT32_MAX))
-    return delete p, fail(PFX_ERANGE, "pfx_plan_create: too many decode pieces");
+    return fail(PFX_ERANGE, "pfx_plan_create: too many decode pieces");
   for (int32_t k : seg_order) {
     const Piece& pc = pcs[k];
     p->seg_shape.row_vecs = std::max(p->seg_shape.row_vecs, (dit[pc.item].rows + 3) / 4);
@@ -767,7 +785,7 @@ extern "C" int pfx_plan_create(const pfx_pool* pool, const pfx_prefix_table* pt,
   if (int64_t(nitems) > kComputeUnits && int64_t(nitems) <= kResidentExtend && beside == 0 && kComputeUnits % hkv == 0)
     std::reverse(xrank.begin() + kComputeUnits / hkv, xrank.end());
   if (nitems + wide_order.size() > size_t(INT32_MAX))
-    return delete p, fail(PFX_ERANGE, "pfx_plan_create: too many extend blocks");
+    return fail(PFX_ERANGE, "pfx_plan_create: too many extend blocks");
   p->n_extend_items = static_cast<int32_t>(nitems);
   p->num_wide = static_cast<int32_t>(wide_order.size());
 
@@ -1062,8 +1080,10 @@ extern "C" int pfx_plan_create(const pfx_pool* pool, const pfx_prefix_table* pt,
     }
   }
 
-  *out = p;
+  *out = owned.release();
   return PFX_OK;
+} catch (...) {
+  return pfx::fail_exception("pfx_plan_create");
 }
 
 extern "C" int pfx_plan_workspace_bytes(const pfx_plan* p, size_t* bytes) {
