@@ -191,7 +191,13 @@ def make_pool(num_pages: int, num_kv_heads: int, head_dim: int, k_pages=None, v_
 
 def make_pool8(num_pages: int, num_kv_heads: int, head_dim: int, k_pages=None, v_pages=None,
                scales=None) -> pfx_pool8:
-    """8-bit pool descriptor over uint8 tensors: pages [num_pages][Hkv][16 d], scales [num_pages][Hkv][2]."""
+    """8-bit pool descriptor over uint8 tensors: pages [num_pages][Hkv][16 d], scales [num_pages][Hkv][2].  Smaller ones,
+    or views that are not contiguous, are refused: the kernels would read and write past them."""
+    heads = num_pages * num_kv_heads
+    for t, need in ((k_pages, heads * PFX_PAGE_SIZE * head_dim), (v_pages, heads * PFX_PAGE_SIZE * head_dim),
+                    (scales, 2 * heads)):
+        if t is not None and not (t.dtype is torch.uint8 and t.is_contiguous() and t.numel() >= need):
+            raise ValueError(f"a pool tensor must be contiguous uint8 of at least {need} values")
     return pfx_pool8(num_pages, PFX_PAGE_SIZE, num_kv_heads, head_dim, _ptr(k_pages), _ptr(v_pages), _ptr(scales))
 
 

@@ -44,3 +44,16 @@ def test_no_rows_at_all(reqs):
         B.pfx_step8(pool, plan, x, x, x, x)
     B.pfx_sync_check()
     assert not any(x.any() for x in t)
+
+
+def test_pool_descriptors_refuse_tensors_that_do_not_hold_the_pool():
+    k, v, s = (torch.zeros((5, 2, w), dtype=torch.uint8) for w in (1024, 1024, 2))
+    ok = B.make_pool8(5, 2, 64, k, v, s)
+    assert (ok.k_pages, ok.v_pages, ok.scales) == (k.data_ptr(), v.data_ptr(), s.data_ptr())
+    B.make_pool8(4, 2, 64, k[1:], v[:4], s)  # room behind the pool
+    for bad in ((k[1:], v, s), (k, v[:, :1], s), (k, v, s[:4]), (k.int(), v, s), (k, v, s.float()),
+                (k, torch.zeros((5, 1024, 2), dtype=torch.uint8).transpose(1, 2), s)):
+        with pytest.raises(ValueError, match="contiguous uint8"):
+            B.make_pool8(5, 2, 64, *bad)
+    with pytest.raises(ValueError, match="contiguous uint8"):
+        B.make_pool8(5, 2, 128, k, v, s)
