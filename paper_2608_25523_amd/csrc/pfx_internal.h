@@ -75,8 +75,10 @@ static_assert(sizeof(Chunk) == 32, "Chunk is 8 int32");
 // An extend block that was cut: its nparts states are in slots base,
 // base + 1, ...  A slot holds, in fp32, the block's unnormalised accumulators
 // as the four waves' lanes hold them (32 columns a wave: [wave][16-column
-// block][dims 16 blk ..][lane] f32x4, 128 D floats) and the pair (m, l) of
-// each of its 128 columns.
+// block][dims 16 blk ..][lane] f32x4, 128 D floats; in plans of an 8-bit pool
+// [wave][32-dim block b][q][lane] f32x4, where lane (col, g) holds dims D / 2 (q
+// / 2) + 16 b + 8 (q % 2) + 4 g .. + 3 of column 32 wave + col) and the pair
+// (m, l) of each of its 128 columns.
 struct ChunkMerge {
   int32_t item, base, nparts, pad;
 };
@@ -140,7 +142,8 @@ struct SegShape {
 // slot's rows hold 16-byte units in unit-major order: unit u = 4 p + grp of
 // row g (dims 32 p + 4 grp .. + 3, then 32 p + 16 + 4 grp .. + 3) at
 // element (u G + g) 8, so that a wave stores each token's G rows as one
-// contiguous run.
+// contiguous run.  In plans of an 8-bit pool a row holds its D accumulators in
+// fp32 as they are, not divided by l, in the order of the dims.
 struct MergeHead {
   int32_t base;
   int32_t nparts;

@@ -174,8 +174,8 @@ __device__ __forceinline__ void quantize_block(const uint16_t* rows, size_t stri
 
 // The touched pages of an append: one wave per (page, KV head, K or V).  Bound
 // by the chain record -> rows and old block -> store for a decode batch (64
-// tokens, 8 KV heads, D = 128: 4.4 us), by HBM for prompts (36864 tokens: 49 us,
-// 4.6 TB/s of rows read and blocks written).
+// tokens, 8 KV heads, D = 128: 4.5 us), by HBM for prompts (36864 tokens: 49-57 us,
+// 4.0-4.6 TB/s of rows read and blocks written).
 template <int D>
 __global__ __launch_bounds__(256) void append8_kernel(const PageWrite* writes, size_t units, const uint16_t* k_new,
                                                       const uint16_t* v_new, unsigned char* k8, unsigned char* v8,
@@ -572,10 +572,11 @@ __device__ __forceinline__ void step8(State8<D, NB>& st, Tile8<D>& tile, uint32_
 // 2048 tokens, 32 query and 8 KV heads, D = 128).  Two steps' loads, 64 (D = 128)
 // or 32 bytes a lane each, are in flight while a third is multiplied.
 //
-// Bound by HBM: that batch's 56 MB take 15.2 us (3.7 TB/s; few enough bytes that
-// the record -> block ids -> first loads chain and the joins show), 16 agents
+// Bound by HBM: that batch's 56 MB take 15.2-16.5 us (3.4-3.7 TB/s; few enough bytes
+// that the record -> block ids -> first loads chain and the joins show), 16 agents
 // with uneven requests, 398 MB, 85.6 us (4.65 TB/s, of 4.9 that a large copy
-// reaches).  The joins' results go to merge8_kernel in fp32.
+// reaches); calls over pools in turn, with nothing of them left in the last-level
+// cache, 23.4 and 98 us with the merge instead of 18.4 and 91.  The joins' results go to merge8_kernel in fp32.
 // ---------------------------------------------------------------------------
 template <int D>
 __device__ __forceinline__ void load_tile8(Tile8<D>& t, const Attn8Args& x, int b0, int b1, int lane) {

@@ -94,6 +94,9 @@ constexpr int32_t kLeastPieceSteps = 3;
 // 11.1, 10.8, 10.9; 32 of four 21.0, 16.9, 13.5, 13.3.  The longer lengths above
 // are the best here too (d 128): 128 requests of four agents, 21928 steps, 35.0
 // at 24, 32.8 at 32, 38.2 at 64; 256 of 16, 56448 steps, 97.5 at 32, 90.5 at 64.
+// At d = 64, 12 steps and 16: 4 requests of one agent over 2048 8.2 and 8.7, 8 of
+// two over 4096 9.9 and 9.7, 64 of one over 2048 12.3 and 13.1, 24 of one over 8192
+// 16.1 and 14.5.
 constexpr int32_t kLeastPieceSteps8 = 12;
 // Workgroups resident at once on 256 compute units, by the registers: two on
 // each at d = 128; at d = 64 four of the kernel that runs only pieces on the

@@ -3,9 +3,10 @@
 //   x <- x / sqrt(mean(x^2) + eps) * w;  (x_a, x_b) <- the pair turned by
 //   position * inv_freq.
 // Every value is read once and written once: the pass is bound by HBM (36864
-// tokens of 32 + 8 heads, D = 128, 755 MB: 135-139 us, 5.4 TB/s; a copy of 2 GiB reaches
-// 5.1), for few tokens by the chain position -> angle -> rotation (one
-// token 3.3 us, 64 4.4, 1999 6.9).  D / 16 lanes hold a head,
+// tokens of 32 + 8 heads, D = 128, 755 MB: 135-139 us, 5.4-5.6 TB/s, over buffers of
+// 4.5 GB in turn too; copies of 377 MB in turn reach 5.3, one of 4 GiB 4.95), for few
+// tokens by the chain position -> angle -> rotation (one token 3.4 us, 64 4.4; 1999
+// with D = 64 6.3-6.9).  D / 16 lanes hold a head,
 // 16 values each, as two 16-byte vectors that lie half a rotation apart, so a
 // lane owns its pairs.  The workgroup computes each token's rotary_dim / 2
 // angles once, in LDS, for all of its heads.
