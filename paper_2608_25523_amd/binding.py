@@ -388,14 +388,16 @@ def _check_rows(plan: Plan, which: int, a, b, lse=None):
 
 def pfx_append_kv8(pool: pfx_pool8, plan: Plan, k_new, v_new, stream=None):
     _check_rows(plan, 0, k_new, v_new)
-    rc = LIB.pfx_append_kv8(pool, plan.h, _ptr(k_new), _ptr(v_new), _call_stream(stream, k_new, v_new))
+    rc = LIB.pfx_append_kv8(pool, plan.h, None if k_new is None else k_new.data_ptr(),
+                            None if v_new is None else v_new.data_ptr(), _call_stream(stream, k_new, v_new))
     if rc:
         _check(rc)
 
 
 def pfx_attention8(pool: pfx_pool8, plan: Plan, q, o, lse=None, sm_scale: float = 0.0, stream=None):
     _check_rows(plan, 1, q, o, lse)
-    rc = LIB.pfx_attention8(pool, plan.h, _ptr(q), _ptr(o), _ptr(lse), sm_scale, _call_stream(stream, q, o, lse))
+    rc = LIB.pfx_attention8(pool, plan.h, None if q is None else q.data_ptr(), None if o is None else o.data_ptr(),
+                            None if lse is None else lse.data_ptr(), sm_scale, _call_stream(stream, q, o, lse))
     if rc:
         _check(rc)
 
@@ -403,7 +405,9 @@ def pfx_attention8(pool: pfx_pool8, plan: Plan, q, o, lse=None, sm_scale: float 
 def pfx_step8(pool: pfx_pool8, plan: Plan, k_new, v_new, q, o, lse=None, sm_scale: float = 0.0, stream=None):
     _check_rows(plan, 0, k_new, v_new)
     _check_rows(plan, 1, q, o, lse)
-    rc = LIB.pfx_step8(pool, plan.h, _ptr(k_new), _ptr(v_new), _ptr(q), _ptr(o), _ptr(lse), sm_scale,
+    rc = LIB.pfx_step8(pool, plan.h, None if k_new is None else k_new.data_ptr(),
+                       None if v_new is None else v_new.data_ptr(), None if q is None else q.data_ptr(),
+                       None if o is None else o.data_ptr(), None if lse is None else lse.data_ptr(), sm_scale,
                        _call_stream(stream, k_new, v_new, q, o, lse))
     if rc:
         _check(rc)
